@@ -26,8 +26,10 @@
 // tokens in 22 us, of which the memory takes 8.5.
 //
 // Exactness.  Scores, statistics and sums are in 32 bits; Q is exact in fp16 after a power of two per row (what lies 2^-28 below a
-// row's largest entry is rounded).  P is rounded to fp16 (2^-11 of each weight, against 2^-8 of the bf16 result) after
-// multiplying by the scale and a power of two that keeps a group's scales in fp16's range.  The row's reference is a maximum that is
+// row's largest entry is rounded).  P times a group's scale is rounded to fp16: 2^-11 of each product, against 2^-8 of the bf16 result.  The
+// power of two that keeps these products in fp16's range is a row's own, for each group of channels, and comes from the products and not from the
+// scales: a loud value that the row does not see or hardly weighs takes nothing from the others (one power for all rows, from the
+// scales: values of 1e-4 beside an unseen one of 65504 were off by 13 %).  The row's reference is a maximum, rounded up to a whole number, that is
 // renewed only when a score exceeds it by 6 in the exponent of 2.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -45,9 +47,11 @@ constexpr int kStepTokens = 32;
 // and with half the warps too little latency is hidden.
 constexpr int kWarps = 8, kThreads = kWarps * 32, kCtasPerSm = 2, kRows = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kLazy = 6.f;           // log2 of how far a weight may exceed 1 before the reference is renewed
-constexpr float kMostScale = 512.f;    // the same for scales: weight times scale stays below 2^15 in fp16
-constexpr float kUnsetDown = 1.2676506e30f;  // 2^100, before the first scale: any but 0 exceeds kMostScale
+constexpr float kMostWeight = 64.f;      // how far a weight may exceed 1 before the reference is renewed
+constexpr float kMostProduct = 32768.f;  // the same for weights times scales, which are to be fp16 numbers
+// log2 of a row's power of two before its first product, and at most: the smallest scale with a weight of 2^-25 exceeds kMostProduct, and zeros
+// that have joined the sums stay in range
+constexpr int kMostDown = 64;
 constexpr int kSegmentCost = 2;        // what beginning and ending a segment costs, in steps
 constexpr float kFloor = -3e38f;       // the reference before any key has been seen: below any score
 
@@ -106,6 +110,8 @@ __device__ __forceinline__ float2 half2_of(uint32_t w) { return __half22float2(*
 
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
+// floor(log2 x) of a normal positive number
+__device__ __forceinline__ int exponent(float x) { return (__float_as_int(x) >> 23) - 127; }
 
 // a / b for powers of two whose quotient is a normal number
 __device__ __forceinline__ float over(float a, float b) {
@@ -218,7 +224,7 @@ struct Rolling {
   float acc[NG][4][4];               // O^T: group, nibble, (channel 8g + i, row 2t), (.., 2t + 1), (8g + 4 + i, 2t), ..
   float zero_sum[2][NG];             // this lane's part of sum_j p_j z_jn, since it last joined acc
   float ref[2], sum[2];          // reference; this lane's part of the sum of weights
-  float down[NG];                        // a power of two that V scales are multiplied by
+  float down[2][NG];                 // a power of two that the row's weights times scales are multiplied by
 };
 
 // A warp's place in the work: rows row0 ... row0 + rows - 1 (of the group's heads, position by position) and their keys.
@@ -341,13 +347,14 @@ __device__ __forceinline__ void unpack_queries(float scale_log2, const uint4 (&r
 template <int D>
 __device__ __forceinline__ void clear(Rolling<D> &r) {
 #pragma unroll
-  for (int n = 0; n < D / kGroup; ++n) r.down[n] = kUnsetDown;
-#pragma unroll
   for (int j = 0; j < 2; ++j) {
     r.ref[j] = kFloor;
     r.sum[j] = 0.f;
 #pragma unroll
-    for (int n = 0; n < D / kGroup; ++n) r.zero_sum[j][n] = 0.f;
+    for (int n = 0; n < D / kGroup; ++n) {
+      r.zero_sum[j][n] = 0.f;
+      r.down[j][n] = pow2(kMostDown);
+    }
   }
 #pragma unroll
   for (int n = 0; n < D / kGroup; ++n)
@@ -442,82 +449,75 @@ __device__ __forceinline__ void attend_step(const AttendKernelParams &p, uint32_
           if (!any || !(fabsf(vs[u][h][n]) + fabsf(vz[u][h][n]) <= 3e38f)) vs[u][h][n] = vz[u][h][n] = 0.f;
       }
   }
-  // is a reference or a scale's power of two to be renewed?
-  float w[2][4], top = -INFINITY, top_scale = 0.f, scaled_vs[2][2][NG];
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[u][e] = fmaf(score[u][e], r.factor[e & 1], -r.ref[e & 1]);
-    top = fmax3(top, w[u][0], w[u][1]);
-    top = fmax3(top, w[u][2], w[u][3]);
-#pragma unroll
-    for (int n = 0; n < NG; ++n) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) scaled_vs[u][h][n] = vs[u][h][n] * r.down[n];
-      top_scale = fmax3(top_scale, scaled_vs[u][0][n], scaled_vs[u][1][n]);
-    }
-  }
-  if (__any_sync(0xffffffffu, top > kLazy || top_scale > kMostScale)) {
-    // rows: the new reference is the largest score so far
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float most = fmaxf(fmaxf(score[0][j], score[0][2 + j]), fmaxf(score[1][j], score[1][2 + j]));
-      const float largest = max_over_g(most * r.factor[j]);
-      const float now = fmaxf(r.ref[j], largest), shrink = ex2_approx(r.ref[j] - now);
-      r.ref[j] = now;
-      r.sum[j] *= shrink;
-#pragma unroll
-      for (int n = 0; n < NG; ++n) {
-        r.zero_sum[j][n] *= shrink;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          r.acc[n][i][j] *= shrink;
-          r.acc[n][i][2 + j] *= shrink;
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) w[u][2 * h + j] = fmaf(score[u][2 * h + j], r.factor[j], -now);
-    }
-    // groups: the power of two that brings the largest scale to 2^5 ... 2^6: room for later ones to be eight times as large, and
-    // for weights of 2^-19 to be normal numbers in fp16
-#pragma unroll
-    for (int n = 0; n < NG; ++n) {
-      const float largest = max_over_g(fmaxf(fmaxf(vs[0][0][n], vs[0][1][n]), fmaxf(vs[1][0][n], vs[1][1][n])));
-      if (largest * r.down[n] > kMostScale) {
-        const float now = pow2(127 + 5 - int(__float_as_uint(largest) >> 23)), shrink = over(now, r.down[n]);
-        r.down[n] = now;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) scaled_vs[u][h][n] = vs[u][h][n] * now;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) r.acc[n][i][e] *= shrink;
-      }
-    }
-  }
-  // weights, as B operands
+  // weights, and times scales in fp16 as B operands; is a reference or a power of two to be renewed?
+  float w[2][4], top = 0.f, top_product = 0.f;
   uint32_t pb[2][NG][2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      w[u][e] = ex2_approx(w[u][e]);
-      r.sum[e & 1] += w[u][e];
-    }
+    for (int e = 0; e < 4; ++e) w[u][e] = ex2_approx(fmaf(score[u][e], r.factor[e & 1], -r.ref[e & 1]));
+    top = fmax3(top, w[u][0], w[u][1]);
+    top = fmax3(top, w[u][2], w[u][3]);
 #pragma unroll
     for (int n = 0; n < NG; ++n) {
-      float scaled[4];
+      float product[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        scaled[e] = w[u][e] * scaled_vs[u][e / 2][n];
-        r.zero_sum[e & 1][n] = fmaf(w[u][e], vz[u][e / 2][n], r.zero_sum[e & 1][n]);
+      for (int e = 0; e < 4; ++e) product[e] = w[u][e] * r.down[e & 1][n] * vs[u][e / 2][n];
+      top_product = fmax3(top_product, product[0], product[1]);
+      top_product = fmax3(top_product, product[2], product[3]);
+      pb[u][n][0] = pack_half2(product[0], product[1]);
+      pb[u][n][1] = pack_half2(product[2], product[3]);
+    }
+  }
+  if (__any_sync(0xffffffffu, top > kMostWeight || top_product > kMostProduct)) {
+    // A row's new reference is a whole number, the largest score so far rounded up.  Its power of two follows, so that a value whose weight has
+    // become small leaves the room to others; then, if a product is still too large, it is the one that brings the largest of this step
+    // to 2^5 ... 2^6: room for later ones to be 2^9 times as large, and a product of 2^-19 of it is a normal number in fp16.
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float most = fmaxf(fmaxf(score[0][j], score[0][2 + j]), fmaxf(score[1][j], score[1][2 + j]));
+      const float now = fmaxf(r.ref[j], ceilf(max_over_g(most * r.factor[j]))), rise = now - r.ref[j], shrink = ex2_approx(-rise);
+      r.ref[j] = now;
+      r.sum[j] *= shrink;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[u][2 * h + j] = ex2_approx(fmaf(score[u][2 * h + j], r.factor[j], -now));
+#pragma unroll
+      for (int n = 0; n < NG; ++n) {
+        r.zero_sum[j][n] *= shrink;
+        const float largest = max_over_g(fmaxf(fmaxf(w[0][j] * vs[0][0][n], w[0][2 + j] * vs[0][1][n]),
+                                               fmaxf(w[1][j] * vs[1][0][n], w[1][2 + j] * vs[1][1][n])));
+        const int was = exponent(r.down[j][n]);
+        int is = min(was + int(fminf(rise, 300.f)), kMostDown);
+        if (largest * pow2(is) > kMostProduct) is = 5 - exponent(largest);
+        r.down[j][n] = pow2(is);
+        const float by = ex2_approx(float(is - was) - rise);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          r.acc[n][i][j] *= by;
+          r.acc[n][i][2 + j] *= by;
+        }
       }
-      pb[u][n][0] = transpose8x8(pack_half2(scaled[0], scaled[1]));
-      pb[u][n][1] = transpose8x8(pack_half2(scaled[2], scaled[3]));
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int n = 0; n < NG; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          pb[u][n][h] = pack_half2(w[u][2 * h] * r.down[0][n] * vs[u][h][n], w[u][2 * h + 1] * r.down[1][n] * vs[u][h][n]);
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.sum[e & 1] += w[u][e];
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.zero_sum[e & 1][n] = fmaf(w[u][e], vz[u][e / 2][n], r.zero_sum[e & 1][n]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) pb[u][n][h] = transpose8x8(pb[u][n][h]);
     }
   }
   // values
@@ -546,9 +546,9 @@ template <int D>
 __device__ __forceinline__ void join_zeros(Rolling<D> &r) {
 #pragma unroll
   for (int n = 0; n < D / kGroup; ++n) {
-    const float unit = r.down[n] * pow2(-24);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
+      const float unit = r.down[j][n] * pow2(-24);
       const float z = sum_over_g(r.zero_sum[j][n]);
       r.zero_sum[j][n] = 0.f;
 #pragma unroll
@@ -562,7 +562,7 @@ __device__ __forceinline__ void join_zeros(Rolling<D> &r) {
 // Channels 64 m + 8 g ... + 7 of row 2t + j, times `by`.
 template <int D>
 __device__ __forceinline__ void result_of(const Rolling<D> &r, int m, int j, float by, float (&o)[8]) {
-  const float a = over(pow2(24), r.down[m]) * by, a16 = a * 0.0625f, z = r.zero_sum[j][m] * by;
+  const float a = over(pow2(24), r.down[j][m]) * by, a16 = a * 0.0625f, z = r.zero_sum[j][m] * by;
 #pragma unroll
   for (int y = 0; y < 2; ++y)
 #pragma unroll
