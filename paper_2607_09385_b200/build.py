@@ -11,7 +11,7 @@ LIB_PATH = os.path.join(HERE, "libsteel_attn.so")
 SOURCES = ("steel_attn.cu", "steel_kernel.cu", "steel_noalloc.cu", "steel_host.cu", "steel_planner.cpp",
            "steel_cache.cu", "steel_cache_tokens.cu", "steel_cache_attend.cu", "steel_cache_pages.cu")
 HEADERS = ("sm100_ptx.cuh", "steel_bitmap.h", "steel_kernel.h", "steel_plan.h", "steel_planner.h", "steel_wait.cuh",
-           "steel_cache.cuh")
+           "steel_cache.cuh", "steel_cache_wait.cuh")
 PUBLIC_HEADERS = ("steel_attn.h", "steel_cache.h")
 NVCC_FLAGS = ("-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC", "-cudart", "static")

@@ -36,6 +36,7 @@
 
 #include "sm100_ptx.cuh"
 #include "steel_cache.cuh"
+#include "steel_cache_wait.cuh"
 
 namespace steel {
 
@@ -742,8 +743,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
         if (i >= 0) {
           const uint32_t nth = filled + i;
           if (!wait_full(bars_at + (nth % S) * 8, nth / S & 1)) {
-            // the copies in flight are awaited, with the same bound, before anything else uses their place
-            for (int j = i + 1; j < min(i + S, steps); ++j) wait_full(bars_at + (filled + j) % S * 8, (filled + j) / S & 1);
+            await_copies<S>(i, steps, [&](int j) { wait_full(bars_at + (filled + j) % S * 8, (filled + j) / S & 1); });
             if (lane == 0) report(p.c.status, STEEL_ERR_TIMEOUT);
             dead = true;
             break;
