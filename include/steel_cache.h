@@ -178,6 +178,13 @@ steel_status_t steel_cache_free(steel_cache_t *cache, int32_t batch, const int32
  */
 steel_status_t steel_cache_compact(steel_cache_t *cache, int32_t *live, void *cuda_stream);
 
+/*
+ * Test hook for attend's bounded wait of one CTA for the others' parts of a sequence: in this cache's following calls it ends after
+ * `cycles` SM cycles (0: after one look; < 0: the default, about two seconds; at most 2^46).  The kernel then returns normally, the output is
+ * undefined and steel_cache_last_status reports STEEL_ERR_TIMEOUT.  A captured call keeps the bound that it was captured with.
+ */
+steel_status_t steel_cache_debug_wait(steel_cache_t *cache, int64_t cycles);
+
 /* Synchronise `cuda_stream`, then report and clear the status word. */
 steel_status_t steel_cache_last_status(steel_cache_t *cache, void *cuda_stream);
 

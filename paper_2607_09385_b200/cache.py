@@ -16,7 +16,7 @@ STEEL_ERR_NO_PAGES = 6
 EXPORTS = (
     "steel_cache_sizes", "steel_cache_create", "steel_cache_destroy", "steel_cache_reset", "steel_cache_extend",
     "steel_cache_append", "steel_cache_read", "steel_cache_attend", "steel_cache_attend_workspace", "steel_cache_fork",
-    "steel_cache_free", "steel_cache_compact", "steel_cache_last_status",
+    "steel_cache_free", "steel_cache_compact", "steel_cache_debug_wait", "steel_cache_last_status",
 )
 
 _i32, _i64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
@@ -68,6 +68,7 @@ def load_library():
     lib.steel_cache_fork.argtypes = [_vp, _i32, _vp, _vp, _vp]
     lib.steel_cache_free.argtypes = [_vp, _i32, _vp, _vp, _vp]
     lib.steel_cache_compact.argtypes = [_vp, _vp, _vp]
+    lib.steel_cache_debug_wait.argtypes = [_vp, _i64]
     lib.steel_cache_last_status.argtypes = [_vp, _vp]
     for name in EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
@@ -96,6 +97,11 @@ def steel_cache_create(params: CacheParams, memory: CacheMemory) -> int:
 
 def steel_cache_destroy(handle) -> None:
     _check(load_library().steel_cache_destroy(handle), "steel_cache_destroy")
+
+
+def steel_cache_debug_wait(handle, cycles: int) -> None:
+    """Test hook: the bound of attend's wait for other CTAs' parts (0: one look; < 0: the default)."""
+    _check(load_library().steel_cache_debug_wait(handle, cycles), "steel_cache_debug_wait")
 
 
 # The layouts of steel_cache_tensor_t and steel_cache_attend_t: one call fills a structure (field by field costs 1 us more)

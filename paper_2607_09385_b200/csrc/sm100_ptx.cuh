@@ -264,6 +264,22 @@ __device__ __forceinline__ int atomic_add_acq_rel(int *p, int v) {
   asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
   return old;
 }
+// Flags in global memory.  What the thread has seen before, its warp's writes after a barrier among it, is seen by who reads the new value.
+__device__ __forceinline__ uint64_t exchange_release(uint64_t *p, uint64_t value) {
+  uint64_t old;
+  __threadfence();
+  asm volatile("atom.exch.release.gpu.global.b64 %0, [%1], %2;" : "=l"(old) : "l"(p), "l"(value) : "memory");
+  return old;
+}
+__device__ __forceinline__ uint64_t load_acquire(const uint64_t *p) {
+  uint64_t seen;
+  asm volatile("ld.acquire.gpu.global.b64 %0, [%1];" : "=l"(seen) : "l"(p) : "memory");
+  return seen;
+}
+__device__ __forceinline__ uint64_t compare_and_swap(uint64_t *p, uint64_t expected, uint64_t value) {
+  return atomicCAS(reinterpret_cast<unsigned long long *>(p), static_cast<unsigned long long>(expected),
+                   static_cast<unsigned long long>(value));
+}
 __device__ __forceinline__ float ex2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -26,6 +26,7 @@ struct steel_cache {
   steel_cache_memory_t memory;
   CacheView view;  // pool of layer 0
   int device, sms;
+  long long wait_cycles;  // of attend, for another CTA's part
 };
 
 namespace {
@@ -135,6 +136,7 @@ steel_status_t steel_cache_create(const steel_cache_params_t *params, const stee
   c->memory = *m;
   c->device = device;
   c->sms = sms;
+  c->wait_cycles = kWaitCycles;
   c->view = CacheView{static_cast<unsigned char *>(m->pool), m->table, m->lens, m->refs, m->status,
                       sizes.page_bytes * params->pages, sizes.page_bytes, params->layers, params->pages,
                       log2_of(params->page_tokens), params->heads_kv, params->slots, params->max_pages};
@@ -217,7 +219,7 @@ steel_status_t steel_cache_attend(steel_cache_t *c, const steel_cache_attend_t *
       a->workspace_bytes < steel_cache_attend_workspace(c, a->batch, a->heads_q, a->seq_q))
     return STEEL_ERR_INVALID_ARG;
   AttendProblem p{CacheBatch{a->slots, a->counts, a->batch}, a->heads_q, a->seq_q, c->params.head_dim, a->flags, a->scale,
-                  a->window, q, a->o, a->lse, static_cast<unsigned char *>(a->workspace)};
+                  a->window, q, a->o, a->lse, static_cast<unsigned char *>(a->workspace), c->wait_cycles};
   return launched(launch_attend(layer_view(c, a->layer), p, c->sms, static_cast<cudaStream_t>(cuda_stream)));
 }
 
@@ -243,6 +245,12 @@ steel_status_t steel_cache_compact(steel_cache_t *c, int32_t *live, void *cuda_s
   if (!aligned(live, 4)) return STEEL_ERR_INVALID_ARG;
   return launched(launch_compact(c->view, c->params.head_dim, c->memory.scratch, live, c->sms,
                                  static_cast<cudaStream_t>(cuda_stream)));
+}
+
+steel_status_t steel_cache_debug_wait(steel_cache_t *c, int64_t cycles) {
+  if (!c) return STEEL_ERR_INVALID_ARG;
+  c->wait_cycles = cycles < 0 ? kWaitCycles : std::min<long long>(cycles, 1ll << 46);
+  return STEEL_OK;
 }
 
 steel_status_t steel_cache_last_status(steel_cache_t *c, void *cuda_stream) {

@@ -25,8 +25,8 @@ struct CacheView {
 
 constexpr long long kWaitCycles = 1ll << 32;  // the bound of a wait on the device: about two seconds
 
-// Numbers that memory does not hold by chance, another for each launch: a flag in memory that nobody has cleared is set only if it equals its
-// launch's.  (A launch in a graph keeps its number; who has read a flag takes it away.)
+// Odd numbers that memory does not hold by chance, another for each launch: a flag in memory that nobody has cleared is set only if it equals its
+// launch's.  (A launch in a graph keeps its number: steel_cache_wait.cuh.)
 uint64_t next_token();
 
 struct Rows {  // steel_cache_tensor_t
@@ -91,6 +91,7 @@ struct AttendProblem {
   void *o;
   float *lse;
   unsigned char *workspace;
+  long long wait_cycles;
 };
 bool attend_fits(const CacheView &c, int batch, int heads_q, int seq_q);  // the work counts within 32 bits
 int64_t attend_workspace(int head_dim, int sms);

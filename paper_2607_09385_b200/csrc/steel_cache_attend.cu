@@ -78,6 +78,7 @@ struct AttendKernelParams {
   float *parts;      // [grid][rows][head_dim], then reference and sum of each row: a segment's part in a CTA that does not end it
   uint64_t *flags;   // [grid][rows]: `token` once the row is there
   uint64_t token;    // of this launch alone
+  long long wait_cycles;  // the bound of a wait for another CTA's part
   int32_t group, seq_q, row_tiles, window, mask;
   float scale_log2;
   FastDivisor by_group, by_row_tiles, by_warps;
@@ -151,21 +152,6 @@ __device__ __forceinline__ bool wait_full(uint32_t bar, uint32_t parity) {
     }
   }
   return true;
-}
-
-// A row of a part is handed over: written by the warp before, read by the one that has seen the flag.
-__device__ __forceinline__ void set_flag(uint64_t *flag, uint64_t token) {
-  __threadfence();
-  asm volatile("st.release.gpu.global.b64 [%0], %1;" ::"l"(flag), "l"(token) : "memory");
-}
-__device__ __forceinline__ bool wait_flag(const uint64_t *flag, uint64_t token) {
-  const long long since = clock64();
-  for (;;) {
-    uint64_t seen;
-    asm volatile("ld.acquire.gpu.global.b64 %0, [%1];" : "=l"(seen) : "l"(flag) : "memory");
-    if (seen == token) return true;
-    if (clock64() - since > kWaitCycles) return false;
-  }
 }
 
 // The value of lane 0, which the compiler then knows to be the same in all lanes: branches on it need no code for warps that part.
@@ -875,7 +861,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
         for (int c = 0; c < V; ++c) part[row * D + lane * V + c] = o[c];
         if (lane == 0) part[R * D + row] = top, part[R * D + R + row] = l;
         __syncwarp();
-        if (lane == 0) set_flag(p.flags + int64_t(blockIdx.x) * R + row, p.token);
+        if (lane == 0) hand_over(p.flags + int64_t(blockIdx.x) * R + row, p.token);
       }
     }
     task += max(rows, 0);
@@ -887,9 +873,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   const int64_t first_other = int64_t(blockIdx.x) - others;
   const float *parts = p.parts + first_other * part_floats(R, D);
   for (int i = threadIdx.x; i < others * rows; i += kThreads) {
-    uint64_t *flag = p.flags + (first_other + i / rows) * R + i % rows;
-    if (!wait_flag(flag, p.token)) report(p.c.status, STEEL_ERR_TIMEOUT);
-    *flag = 0;  // a replay of the launch has the same token
+    if (!take_over(p.flags + (first_other + i / rows) * R + i % rows, p.token, p.wait_cycles)) report(p.c.status, STEEL_ERR_TIMEOUT);
   }
   __syncthreads();
   const int each_row = max(kWarps / max(rows, 1), 1);  // warps that share a row's parts
@@ -991,6 +975,7 @@ cudaError_t launch_attend(const CacheView &c, const AttendProblem &a, int sms, c
   kp.flags = reinterpret_cast<uint64_t *>(a.workspace);
   kp.parts = reinterpret_cast<float *>(a.workspace + flags_bytes(grid));
   kp.token = next_token();
+  kp.wait_cycles = a.wait_cycles;
   kp.group = group;
   kp.seq_q = a.seq_q;
   kp.row_tiles = (group * a.seq_q + kRows - 1) / kRows;

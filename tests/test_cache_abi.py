@@ -123,3 +123,7 @@ def test_reference_model_shares_copies_and_compacts():
     assert m.free([2], [3]) == "ok" and m.rows[2] == [0] and m.free([1], [0]) == "ok"
     assert m.extend([0], [17]) == "ok" and m.rows[0] == [1, 2] and m.free([2], [0]) == "ok"
     assert m.compact() == (2, {2: 0}) and m.rows[0] == [1, 0]
+
+
+def test_debug_wait_refuses_no_cache():
+    assert C.load_library().steel_cache_debug_wait(None, 0) == B.STEEL_ERR_INVALID_ARG

@@ -1,4 +1,5 @@
-"""What the cache's attention does when a bounded wait has expired, on the host: no copy is left in flight.  CPU only."""
+"""What the cache's attention does when a bounded wait has expired, on the host: no copy is left in flight, and a part that came
+too late is not taken by the next execution of a captured launch.  CPU only."""
 import os
 import subprocess
 
@@ -12,7 +13,7 @@ def cache_wait(tmp_path_factory, repo_root):
     return exe
 
 
-@pytest.mark.parametrize("what", ["ring"])
+@pytest.mark.parametrize("what", ["ring", "replays", "threads"])
 def test_expired_waits(cache_wait, what):
     out = subprocess.run([cache_wait, what], capture_output=True, text=True, timeout=120)
     assert out.returncode == 0, out.stdout
