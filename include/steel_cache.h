@@ -114,7 +114,7 @@ steel_status_t steel_cache_extend(steel_cache_t *cache, int32_t batch, const int
 /*
  * Quantise the last counts[i] tokens (NULL = seq) of each slot, for which extend has made room: token j < counts[i] of the
  * batch's sequence i (0 <= counts[i] <= seq <= 2^30) goes to position lens[slot] - counts[i] + j.  Of k and v only those rows are read.
- * No fork of the slot between extend and append: both would write the same page.
+ * A token whose page other table entries name too (refs > 1: the slot was forked and not extended) is not written, and reported.
  */
 steel_status_t steel_cache_append(steel_cache_t *cache, int32_t layer, int32_t batch, const int32_t *slots,
                                   const int32_t *counts, int32_t seq, const steel_cache_tensor_t *k,

@@ -194,6 +194,16 @@ __device__ __forceinline__ unsigned char *unit_in(const CacheView &c, int page, 
   return c.pool + page * c.page_bytes + (int64_t(head) * units + (first / kUnitTokens & (units - 1))) * bytes;
 }
 
+// The same for writing: a page that other entries name too is left alone.
+__device__ __forceinline__ unsigned char *own_unit_in(const CacheView &c, int page, int first, int head, int bytes, int lane) {
+  unsigned char *unit = unit_in(c, page, first, head, bytes, lane);
+  if (unit && c.refs[page] > 1) {
+    if (lane == 0) report(c.status, STEEL_ERR_INVALID_ARG);
+    return nullptr;
+  }
+  return unit;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kWarps * 32, 7) append_kernel(CacheView c, CacheBatch b, int seq, int units_a_head, Rows k, Rows v) {
   constexpr int NG = D / kGroup;
@@ -208,7 +218,7 @@ __global__ void __launch_bounds__(kWarps * 32, 7) append_kernel(CacheView c, Cac
   const int start = len - count, first = (start / kUnitTokens + nth) * kUnitTokens;
   if (len < 0 || first >= len || count == 0) return;
   const int from = max(start - first, 0), to = min(len - first, kUnitTokens);
-  unsigned char *out = unit_in(c, page_of(c, slot, first), first, head, unit_bytes(D), lane);
+  unsigned char *out = own_unit_in(c, page_of(c, slot, first), first, head, unit_bytes(D), lane);
   if (!out) return;
   const bool whole = from == 0 && to == kUnitTokens;
 
@@ -327,8 +337,7 @@ __global__ void __launch_bounds__(kWarps * 32) append_few_kernel(CacheView c, Ca
   const int len = checked_length(c, b, i, seq, lane, work == 0, slot, count);
   if (len < 0 || j >= count) return;
   const int pos = len - count + j, token = pos % kUnitTokens, m = lane % (D / 4);
-  unsigned char *out = unit_in(c, page_of(c, slot, pos), pos, head, unit_bytes(D), lane);
-  if (!out) return;
+  // under way while the page and its count are looked up
   const unsigned char *rk = k.data + i * k.batch + head * k.head + j * k.seq + m * 8;
   const unsigned char *rv = v.data + i * v.batch + head * v.head + j * v.seq + m * 8;
   constexpr int kPasses = D == 64 ? 1 : 2;
@@ -339,6 +348,8 @@ __global__ void __launch_bounds__(kWarps * 32) append_few_kernel(CacheView c, Ca
     x[0] = *reinterpret_cast<const uint2 *>(rk);
     x[kPasses - 1] = *reinterpret_cast<const uint2 *>(rv);
   }
+  unsigned char *out = own_unit_in(c, page_of(c, slot, pos), pos, head, unit_bytes(D), lane);
+  if (!out) return;
 #pragma unroll 1
   for (int pass = 0; pass < kPasses; ++pass) {
     const uint32_t w[2] = {pass ? x[kPasses - 1].x : x[0].x, pass ? x[kPasses - 1].y : x[0].y};
