@@ -114,7 +114,8 @@ class SteelCache:
     """Owner of one cache on a CUDA device (the current one by default).
 
     ``pool``, ``table``, ``lens`` and ``refs`` are torch tensors in the layout of the header; the methods enqueue
-    their kernels on torch's current stream of that device.  Index arguments (``slots``, ``counts``, ``begin``,
+    their kernels on torch's current stream of that device, which has to be the current one (``torch.cuda.device``): they
+    refuse with STEEL_ERR_INVALID_ARG otherwise.  Index arguments (``slots``, ``counts``, ``begin``,
     ``keep``, ``src``, ``dst``) are int32 CUDA tensors; what is wrong in them is found on the device and reported by
     ``last_status``.  Calls on one object from several host threads have to be serialised.  A step of a decoder:
 
@@ -128,6 +129,7 @@ class SteelCache:
         import torch
         self.params = CacheParams(layers, pages, page_tokens, heads_kv, head_dim, slots, max_pages)
         size = steel_cache_sizes(self.params)
+        assert device is None or torch.device(device).type == "cuda", "device: a CUDA device"
         index = None if device is None else torch.device(device).index
         device = torch.device("cuda", torch.cuda.current_device() if index is None else index)
         self.device_index = device.index
@@ -141,6 +143,7 @@ class SteelCache:
         memory = CacheMemory(*(x.data_ptr() for x in (self.pool, self.table, self.lens, self.refs, self.status, self._scratch)))
         with torch.cuda.device(device):
             self.handle = steel_cache_create(self.params, memory)
+            _check(load_library().steel_cache_reset(self.handle, binding._stream_getter()(device.index)), "steel_cache_reset")
         # what every call needs, looked up once: a decode step's calls are as short as this path (append of one token to 64
         # sequences: 6.9 us of host time before, of which 2.3 are the launch)
         self._lib, self._stream = load_library(), binding._stream_getter()
@@ -149,7 +152,6 @@ class SteelCache:
         self._workspaces = {}  # bytes by (heads_q, seq_q)
         self._empty, self._bf16, self._i32, self._f32 = torch.empty, torch.bfloat16, torch.int32, torch.float32
         self._device = device
-        self.reset()
 
     def _index(self, x, n, what):
         """Address of an index tensor of n entries (None: no tensor)."""
