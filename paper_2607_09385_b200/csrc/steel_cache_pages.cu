@@ -1,11 +1,14 @@
 // Page management of the 4-bit cache, on the device: extend, fork, free, compact (include/steel_cache.h).
 //
-// Who owns what is decided by one cluster of eight CTAs (or one CTA where there is little to look at: a cluster's barriers cost about half a
-// microsecond each), which can wait for one another: each checks the whole batch for itself, all reads come before a cluster
-// barrier and all writes after it, so that a call either is done or changes nothing, and rows may be read and written by the
-// same call (fork).  A page is free where refs is 0, and the lowest free pages are given out in the order of
-// the batch, a lane a page: every result is fixed by the call's inputs, whatever the timing.  Bound by the latency of its dependent reads (slot ->
-// length -> last page -> refs) and the barriers.
+// Who owns what is decided by one cluster of eight CTAs, which can wait for one another: each checks the whole batch for itself and nothing
+// is changed unless all of it is as it should be, so that a call either is done or changes nothing.  What another CTA of the cluster reads
+// for its answer is changed behind a cluster barrier only: extend takes free pages, writes table entries and counts behind one and lengths
+// behind another; fork takes down all rows (and counts them, by atomics that nobody reads) before it overwrites any, so that rows may be read and
+// written by the same call; free checks all lengths before it changes any.  A page is free where refs is 0, and the lowest free pages are given out
+// in the order of the batch, a lane a page: every result is fixed by the call's inputs, whatever the timing.  Bound by the latency of its dependent
+// reads (slot -> length -> last page -> refs) and the barriers.  One CTA, without the barriers between CTAs, is no variant of its own: a fork of up to
+// 512 table entries takes 3.7 us by one and 3.9 by eight, of 16384 24 to 32 and 6 to 7; extend for 8 sequences 5.5 and 5.6, for 256 10.1 and 7.0;
+// free for 8 1.65 and 1.67, for 256 5.9 and 2.4; compaction's plan over 2048 pages 4.9 and 5.0, over 16384 8.3 and 5.4.
 // Contents move in a kernel of their own on all SMs, bound by memory; it finds its list in scratch memory, and where nothing is to be
 // moved (the usual extend) it returns at once.  (Movers in the same launch as extend's cluster, waiting for its list, saved a launch's 2.3 us
 // of host time and cost 2 us on the device, which is what the steps wait for.)
@@ -20,7 +23,7 @@ namespace steel {
 
 namespace {
 
-constexpr int kMostCtas = 8, kThreads = 512, kWarps = kThreads / 32;
+constexpr int kCtas = 8, kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMoveThreads = 256;
 
 struct Move {
@@ -70,13 +73,11 @@ __device__ __forceinline__ bool named_before(uint32_t *seen, int slot) {
 struct Share {
   int begin, words;  // first page, words of 32 pages
 };
-template <int kCtas>
 __host__ __device__ int share_words(int pages) {
   return ((pages + 31) / 32 + kCtas - 1) / kCtas;
 }
-template <int kCtas>
 __device__ Share share_of(int pages, int rank) {
-  const int words = (pages + 31) / 32, each = share_words<kCtas>(pages);
+  const int words = (pages + 31) / 32, each = share_words(pages);
   const int first = min(words, rank * each);
   return {first * 32, min(words, first + each) - first};
 }
@@ -111,7 +112,6 @@ __device__ void rank_words(Share s, const uint32_t *bits, int *ranks, int *sums,
 }
 
 // Values that the CTAs of the cluster tell one another.  -> those of the lower ranks added up; `total` of all.
-template <int kCtas>
 __device__ int cluster_exclusive(cg::cluster_group &cluster, int *mine, int value, int *total) {
   if (threadIdx.x == 0) *mine = value;
   cluster.sync();
@@ -160,7 +160,6 @@ __device__ __forceinline__ void move_units(const CacheView &c, const Move *moves
 // Shared memory: `before` [n + 1] pages wanted before sequence i, `first` [n] the first table column that gets a page (bit 31: the
 // page that is there now is shared and copied), `copies` [n] copies before i, the bits of seen slots, the free bits and how many free pages
 // of this CTA's share stand before each word of them.
-template <int kCtas>
 __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
     extend_kernel(CacheView c, CacheBatch b, void *scratch) {
   extern __shared__ uint32_t smem[];
@@ -170,14 +169,14 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
   const int n = b.batch, tid = threadIdx.x;
   int *before = reinterpret_cast<int *>(smem), *copies = before + n + 1;
   uint32_t *first = reinterpret_cast<uint32_t *>(copies + n), *seen = first + n, *bits = seen + (c.slots + 31) / 32;
-  int *ranks = reinterpret_cast<int *>(bits + share_words<kCtas>(c.pages));
+  int *ranks = reinterpret_cast<int *>(bits + share_words(c.pages));
   clear_seen(c, seen);
   grid_dependency_wait();
   grid_launch_dependents();
 
   // half of the warps look at the batch, the others at the pages: both are chains of reads
   constexpr int kBatchThreads = kThreads / 2;
-  const Share share = share_of<kCtas>(c.pages, cluster.block_rank());
+  const Share share = share_of(c.pages, cluster.block_rank());
   const int each = (n + kBatchThreads - 1) / kBatchThreads, i0 = tid < kBatchThreads ? min(n, tid * each) : n, i1 = min(n, i0 + each);
   bool good = true;
   long long want = 0;  // pages in the low 40 bits, copies above
@@ -221,7 +220,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
   int here;
   rank_words(share, bits, ranks, int_sums, &here);
   int free_total;
-  const int below = cluster_exclusive<kCtas>(cluster, &told, here, &free_total);  // and the barrier between reads and writes
+  const int below = cluster_exclusive(cluster, &told, here, &free_total);  // and the barrier between reads and writes
   // every CTA has read what it reads, and comes to the same answer
   const bool room = wanted <= free_total;
   if (good && room) {
@@ -262,7 +261,6 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
 }
 
 // ---------------------------------------------------------------------------------------------------------------- fork
-template <int kCtas>
 __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
     fork_kernel(CacheView c, void *scratch, int n, const int32_t *src, const int32_t *dst) {
   extern __shared__ uint32_t smem[];
@@ -318,7 +316,6 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
 }
 
 // ---------------------------------------------------------------------------------------------------------------- free
-template <int kCtas>
 __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) free_kernel(CacheView c, CacheBatch b) {
   extern __shared__ uint32_t smem[];
   cg::cluster_group cluster = cg::this_cluster();
@@ -358,23 +355,22 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) free_k
 // With `live` pages in use, the k-th free page below `live` is the k-th hole, the k-th page in use from `live` up the k-th
 // mover; there are as many of the ones as of the others.  A hole's rank is the free pages before it; a mover's the pages in use before
 // it less those below `live`.
-template <int kCtas>
 __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
     compact_kernel(CacheView c, void *scratch, int32_t *live_out) {
   extern __shared__ uint32_t bits[];
-  int *ranks = reinterpret_cast<int *>(bits + share_words<kCtas>(c.pages));
+  int *ranks = reinterpret_cast<int *>(bits + share_words(c.pages));
   __shared__ int told, told_holes;
   __shared__ int sums[kWarps];
   cg::cluster_group cluster = cg::this_cluster();
   grid_dependency_wait();
   grid_launch_dependents();
   const int tid = threadIdx.x;
-  const Share share = share_of<kCtas>(c.pages, cluster.block_rank());
+  const Share share = share_of(c.pages, cluster.block_rank());
   free_pages(c, share, bits, tid / 32, kWarps);
   __syncthreads();
   int here, free_total;
   rank_words(share, bits, ranks, sums, &here);
-  const int below = cluster_exclusive<kCtas>(cluster, &told, here, &free_total);  // free pages before this CTA's; a barrier too
+  const int below = cluster_exclusive(cluster, &told, here, &free_total);  // free pages before this CTA's; a barrier too
   const int live = c.pages - free_total;
   // holes: free pages below `live`.  One CTA has that page, or all of its pages are on one side.
   int holes_here = live <= share.begin ? 0 : here;
@@ -382,7 +378,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
   if (in_share > 0 && in_share < share.words * 32)
     holes_here = ranks[in_share / 32] + __popc(bits[in_share / 32] & ((1u << (in_share % 32)) - 1u));
   int holes;
-  cluster_exclusive<kCtas>(cluster, &told_holes, holes_here, &holes);
+  cluster_exclusive(cluster, &told_holes, holes_here, &holes);
 
   Move *moves = moves_of(scratch);
   int32_t *rank_of = reinterpret_cast<int32_t *>(moves + (c.pages + 1) / 2);
@@ -439,12 +435,9 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(CacheView c, void *s
   }
 }
 
-constexpr int kMaxSeenBytes = kMaxSlots / 8, kMaxBitsBytes = 2 * (kMaxCachePages / 8 / kMostCtas + 4);
-int bits_bytes(int pages, int ctas) { return 2 * 4 * (ctas == 1 ? share_words<1>(pages) : share_words<kMostCtas>(pages)); }  // and ranks
+constexpr int kMaxSeenBytes = kMaxSlots / 8, kMaxBitsBytes = 2 * (kMaxCachePages / 8 / kCtas + 4);
+int bits_bytes(int pages) { return 2 * 4 * share_words(pages); }  // and ranks
 int seen_bytes(int slots) { return (slots + 31) / 32 * 4; }
-
-// One CTA where it is done with its reads after one round trip: see the header of the file.
-constexpr int kFewPages = 2048, kFewEntries = 16384, kFewSequences = 256;  // extend and compact; fork; free and extend
 
 }  // namespace
 
@@ -456,35 +449,27 @@ int64_t pages_scratch_bytes(int slots, int max_pages, int pages) {
 }
 
 cudaError_t configure_pages() {
-  return cudaFuncSetAttribute(extend_kernel<kMostCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  return cudaFuncSetAttribute(extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               (3 * kMaxSlots + 1) * 4 + kMaxSeenBytes + kMaxBitsBytes);
 }
 
 cudaError_t launch_extend(const CacheView &c, int head_dim, void *scratch, const CacheBatch &b, int sms, cudaStream_t stream) {
-  const int ctas = c.pages <= kFewPages && b.batch <= kFewSequences ? 1 : kMostCtas;
-  const int smem = (3 * b.batch + 1) * 4 + seen_bytes(c.slots) + bits_bytes(c.pages, ctas);
-  const cudaError_t e = launch_overlapping(ctas == 1 ? extend_kernel<1> : extend_kernel<kMostCtas>, dim3(ctas), dim3(kThreads), smem,
-                                           stream, c, b, scratch);
+  const int smem = (3 * b.batch + 1) * 4 + seen_bytes(c.slots) + bits_bytes(c.pages);
+  const cudaError_t e = launch_overlapping(extend_kernel, dim3(kCtas), dim3(kThreads), smem, stream, c, b, scratch);
   if (e != cudaSuccess) return e;
   return launch_overlapping(move_kernel<false>, dim3(sms * 2), dim3(kMoveThreads), 0, stream, c, scratch, unit_bytes(head_dim));
 }
 
 cudaError_t launch_fork(const CacheView &c, void *scratch, int n, const int32_t *src, const int32_t *dst, cudaStream_t stream) {
-  const int ctas = int64_t(n) * c.max_pages <= kFewEntries ? 1 : kMostCtas;
-  return launch_overlapping(ctas == 1 ? fork_kernel<1> : fork_kernel<kMostCtas>, dim3(ctas), dim3(kThreads), seen_bytes(c.slots),
-                            stream, c, scratch, n, src, dst);
+  return launch_overlapping(fork_kernel, dim3(kCtas), dim3(kThreads), seen_bytes(c.slots), stream, c, scratch, n, src, dst);
 }
 
 cudaError_t launch_free(const CacheView &c, const CacheBatch &b, cudaStream_t stream) {
-  const int ctas = b.batch <= kFewSequences ? 1 : kMostCtas;
-  return launch_overlapping(ctas == 1 ? free_kernel<1> : free_kernel<kMostCtas>, dim3(ctas), dim3(kThreads), seen_bytes(c.slots),
-                            stream, c, b);
+  return launch_overlapping(free_kernel, dim3(kCtas), dim3(kThreads), seen_bytes(c.slots), stream, c, b);
 }
 
 cudaError_t launch_compact(const CacheView &c, int head_dim, void *scratch, int32_t *live, int sms, cudaStream_t stream) {
-  const int ctas = c.pages <= kFewPages ? 1 : kMostCtas;
-  const cudaError_t e = launch_overlapping(ctas == 1 ? compact_kernel<1> : compact_kernel<kMostCtas>, dim3(ctas), dim3(kThreads),
-                                           bits_bytes(c.pages, ctas), stream, c, scratch, live);
+  const cudaError_t e = launch_overlapping(compact_kernel, dim3(kCtas), dim3(kThreads), bits_bytes(c.pages), stream, c, scratch, live);
   if (e != cudaSuccess) return e;
   return launch_overlapping(move_kernel<true>, dim3(sms * 8), dim3(kMoveThreads), 0, stream, c, scratch, unit_bytes(head_dim));
 }
