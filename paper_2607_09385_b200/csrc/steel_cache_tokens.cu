@@ -23,7 +23,6 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kReadUnits = 2;  // units a warp when reading: 16K x 8 heads at head_dim 128 in 16.4 us, 17.4 with one; 8 x 300 to 6500 at 64 13.2, 15.2
-constexpr int kFewRows = 8, kFewTokens = 64;  // see takes_few
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -514,18 +513,22 @@ __global__ void __launch_bounds__(kWarps * 32) read_few_kernel(CacheView c, cons
 // Units that `seq` tokens can touch, wherever they begin.
 int units_of(int seq) { return (seq + kUnitTokens - 2) / kUnitTokens + 1; }
 
-// Whether a warp takes a token and not a unit: where tokens are few altogether, because units take longer from their first read to their last
-// write, or a sequence has few, because most of a unit would be idle.  Written and read back, by tokens and by units, heads_kv = 8: at
-// head_dim 128 2 x 48 tokens 4.8 and 9.9 us, 64 x 16 10.2 and 12.4, 64 x 24 12.9 and 12.6; at 64 2 x 32 4.3 and 7.2, 64 x 16 9.2 and 8.3.
-bool takes_few(const CacheView &c, int head_dim, int batch, int seq) {
-  return seq <= kFewRows || int64_t(batch) * seq * c.heads_kv <= kFewTokens * head_dim;
+// Whether a warp takes a token and not a unit: where tokens are few altogether, because units take longer from their first access to their
+// last, or a sequence has few, because most of a unit would be idle.  By tokens and by units, 8 heads, in us:
+//   writing  head_dim 128: 64 x 16 tokens 5.6 and 8.6, 256 x 12 12.8 and 10.1, 512 x 4 9.2 and 15.4, 512 x 8 16.4 and 15.9;
+//            head_dim 64: 32 x 16 2.8 and 5.4, 256 x 12 10.1 and 6.5, 512 x 4 7.3 and 10.3, 512 x 8 12.9 and 9.9
+//   reading  head_dim 128: 64 x 4 2.1 and 2.2, 64 x 8 2.7 and 2.3, 512 x 2 3.9 and 5.2, 512 x 4 5.9 and 5.1;
+//            head_dim 64: 32 x 8 2.0 and 2.0, 64 x 8 2.4 and 2.0, 512 x 2 3.7 and 3.7, 512 x 4 5.8 and 3.7
+bool writes_few(const CacheView &c, int head_dim, int batch, int seq) {
+  return seq <= (head_dim == 64 ? 6 : 8) || int64_t(batch) * seq * c.heads_kv <= 64 * head_dim;
 }
+bool reads_few(const CacheView &c, int batch, int seq) { return seq <= 2 || int64_t(batch) * seq * c.heads_kv <= 2048; }
 
 }  // namespace
 
 cudaError_t launch_append(const CacheView &c, int head_dim, const CacheBatch &b, int seq, const Rows &k, const Rows &v,
                           cudaStream_t stream) {
-  if (takes_few(c, head_dim, b.batch, seq)) {
+  if (writes_few(c, head_dim, b.batch, seq)) {
     const dim3 grid((int64_t(seq) * c.heads_kv + kWarps - 1) / kWarps, b.batch);
     return launch_overlapping(head_dim == 64 ? append_few_kernel<64> : append_few_kernel<128>, grid, dim3(kWarps * 32), 0, stream, c,
                               b, seq, k, v);
@@ -538,7 +541,7 @@ cudaError_t launch_append(const CacheView &c, int head_dim, const CacheBatch &b,
 
 cudaError_t launch_read(const CacheView &c, int head_dim, const int32_t *slots, const int32_t *begin, int batch, int seq,
                         const Rows &k, const Rows &v, cudaStream_t stream) {
-  if (takes_few(c, head_dim, batch, seq)) {
+  if (reads_few(c, batch, seq)) {
     const dim3 grid((int64_t(seq) * c.heads_kv + kWarps - 1) / kWarps, batch);
     return launch_overlapping(head_dim == 64 ? read_few_kernel<64> : read_few_kernel<128>, grid, dim3(kWarps * 32), 0, stream, c,
                               slots, begin, seq, k, v);
