@@ -293,8 +293,8 @@ __device__ __forceinline__ void unpack_queries(float scale_log2, const uint4 (&r
     }
   big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
   big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
-  // the power of two that brings it to 2^14 ... 2^15; kept where the row's factor is finite
-  const int up = big == 0 ? 0 : min(max(14 + 127 - int(big >> 7), -100), 126);
+  // the power of two that brings it to 2^14 ... 2^15 (subnormal ones to less)
+  const int up = big == 0 ? 0 : min(14 + 127 - int(big >> 7), 126);
   const float unit = pow2(up);
   float sum[NG];
 #pragma unroll
@@ -322,7 +322,8 @@ __device__ __forceinline__ void unpack_queries(float scale_log2, const uint4 (&r
     sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
     sum[n] *= pow2(-24);  // in the units of the products with codes
   }
-  const float f = fmaxf(scale_log2 * pow2(24 - up), 1.2e-38f);  // not 0: what is masked is -inf
+  // in two steps: 2^(24 - up) alone may leave the range
+  const float f = fmaxf(scale_log2 * pow2(min(24 - up, 64)) * pow2(max(24 - up - 64, 0)), 1.2e-38f);  // not 0: what is masked is -inf
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     r.factor[j] = __shfl_sync(0xffffffffu, f, (2 * t + j) * 4);

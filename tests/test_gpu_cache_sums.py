@@ -170,3 +170,19 @@ def test_values_that_fall_while_scores_rise(d, rise):
     c.append(0, k, v)
     check_rows(c, q, d ** -0.5, 0)
     c.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size,scale", [(2.0 ** 115, 2.0 ** -118), (2.0 ** 119, 2.0 ** -123), (2.0 ** 125, 2.0 ** -126), (2.0 ** -120, 2.0 ** 120)])
+def test_queries_at_the_ends_of_bf16(d, size, scale):
+    # scores of ordinary size whatever the queries': the largest numbers of bf16 and small ones
+    n = 200
+    c = make_cache(1, 20, 16, 1, d, 1, 20)
+    g = torch.Generator(device="cuda").manual_seed(24)
+    k, v = normal(g, 1, 1, n, d), normal(g, 1, 1, n, d)
+    c.extend(ints([n]))
+    c.append(0, k, v)
+    q = (normal(g, 1, 2, 3, d).float().clamp(-3, 3) / 4 * 2 * size).to(torch.bfloat16)
+    assert torch.isfinite(q).all()
+    check_rows(c, q, scale, CAUSAL)
+    c.close()
