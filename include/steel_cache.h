@@ -33,7 +33,7 @@
  * `status` int32: what went wrong on the device (below).   `scratch`: working memory of the calls that change pages.
  *
  * Batches.  `slots` (DEVICE int32 [batch], NULL = 0, 1, 2, ...) says which slots a call is about.  The calls that
- * write want distinct slots; read and attend take a slot several times.
+ * write want distinct slots; read and attend take a slot several times, in batches of up to 65535 (beyond: STEEL_ERR_UNSUPPORTED).
  *
  * Errors on the device.  A slot outside the cache, a count or length that cannot be, a slot named twice where they
  * have to be distinct, a table entry outside the pool: the status word is set to STEEL_ERR_INVALID_ARG; too few free
@@ -92,7 +92,7 @@ typedef struct {
 steel_status_t steel_cache_sizes(const steel_cache_params_t *params, steel_cache_sizes_t *sizes);
 
 /* Checks the arguments and binds the memory; nothing is allocated on the device and nothing is written there:
- * call steel_cache_reset, or bring table, lens and refs of an earlier cache.  *out is NULL on failure. */
+ * call steel_cache_reset, or bring table, lens and refs of an earlier cache and a status of 0.  *out is NULL on failure. */
 steel_status_t steel_cache_create(const steel_cache_params_t *params, const steel_cache_memory_t *memory,
                                   steel_cache_t **out);
 /* destroy(NULL) is STEEL_OK.  The memory stays the caller's. */
@@ -136,7 +136,7 @@ typedef struct {
   float scale;                          /* finite, > 0                                                                 */
   int64_t window;                       /* > 0, used iff WINDOW                                                        */
   steel_cache_tensor_t q;               /* [batch, heads_q, seq_q, head_dim]                                           */
-  void *o;                              /* bf16 [batch, heads_q, seq_q, head_dim], contiguous, 16-byte aligned          */
+  void *o;                              /* bf16 [batch, heads_q, seq_q, head_dim], contiguous, 16-byte aligned, not q   */
   float *lse;                           /* float32 [batch, heads_q, seq_q] or NULL                                     */
   void *workspace;                      /* 128-byte aligned, of steel_cache_attend_workspace bytes; not shared between  */
   int64_t workspace_bytes;              /* calls that may overlap (graphs captured with it included)                   */
@@ -148,6 +148,10 @@ typedef struct {
  * steel_attn.h with seq_q = counts[b], seq_kv = lens).
  *     O = softmax_j(scale q . k_j) V,  LSE = ln sum_j exp(scale q . k_j);  no visible key: O = 0, LSE = -inf.
  * Scores are meant to be below 2^26 in magnitude: beyond, a weight may leave the range of 32 bits.
+ * What is rounded: a weight times the scale of a group of V to fp16 (2^-11 of it; the power of two beside it is the row's own), O to bf16 (2^-8).
+ * Scores, weights, LSE and all sums are in 32 bits.  Codes are summed apart from zeros for up to 512 tokens at a time, so the first rounding counts
+ * about 2.5 times; that is a third of the second or less.  Matrix products cut their sums off by 2^-23.4 each, one way: 0.02 % of O for each
+ * 32768 tokens that one warp goes through (the whole call's steps are dealt out evenly to about 2400 warps).
  * Rows i >= counts[b] are left as they were.  A key that a query does not see has no influence on it but by rounding, whatever its
  * contents, NaN among them.  For a few queries a sequence: 8 rows (queries times query heads of a KV head) go through the cache together,
  * more rows several times; a long chunk of a prompt is better served by steel_cache_read and steel_attn_run.

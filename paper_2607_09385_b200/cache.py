@@ -149,7 +149,7 @@ class SteelCache:
         self._lib, self._stream = load_library(), binding._stream_getter()
         self._args, self._k, self._v = CacheAttend(), CacheTensor(), CacheTensor()
         self._args_at, self._k_at, self._v_at = (ctypes.addressof(x) for x in (self._args, self._k, self._v))
-        self._workspaces = {}  # bytes by (heads_q, seq_q)
+        self._workspaces = {}  # bytes by (batch, heads_q, seq_q)
         self._empty, self._bf16, self._i32, self._f32 = torch.empty, torch.bfloat16, torch.int32, torch.float32
         self._device = device
 
@@ -188,7 +188,7 @@ class SteelCache:
 
     def append(self, layer, k, v, counts=None, slots=None) -> None:
         """Quantise the newest ``counts[i]`` tokens of each slot from k, v [batch, heads_kv, seq, head_dim] (any strides
-        in multiples of 8)."""
+        in multiples of 8).  Tokens on a page that another slot holds too are not written, and reported."""
         n, seq = self._rows(k, v)
         status = self._lib.steel_cache_append(self.handle, layer, n, self._index(slots, n, "slots"), self._index(counts, n, "counts"),
                                               seq, self._k_at, self._v_at, self._stream(self.device_index))
@@ -207,7 +207,8 @@ class SteelCache:
 
     def attend(self, layer, q, scale, counts=None, slots=None, flags=STEEL_MASK_CAUSAL, window=0, o=None, lse=None,
                want_lse: bool = True):
-        """Attention of the newest tokens' queries [batch, heads_q, seq_q, head_dim] over the cache -> (o, lse)."""
+        """Attention of the newest tokens' queries [batch, heads_q, seq_q, head_dim] over the cache -> (o, lse).  Weights
+        are fp16 numbers beside sums in 32 bits: ``include/steel_cache.h`` says what that costs."""
         shape = q.shape
         n, heads_q, seq, d = shape
         batch_stride, head_stride, seq_stride, one = q.stride()
@@ -224,11 +225,11 @@ class SteelCache:
         else:
             assert lse.dtype is self._f32 and lse.shape == (n, heads_q, seq) and lse.is_contiguous() and lse.get_device() == device, \
                 "lse: float32 [batch, heads, seq], contiguous"
-        need = self._workspaces.get((heads_q, seq))
+        need = self._workspaces.get((n, heads_q, seq))
         if need is None:
             need = self._lib.steel_cache_attend_workspace(self.handle, n, heads_q, seq)
             if need >= 0:
-                self._workspaces[heads_q, seq] = need
+                self._workspaces[n, heads_q, seq] = need
         # of this call alone: calls on several streams, and graphs, do not share it.  (In 16-bit elements: new_empty takes the
         # device from q, which is 0.3 us shorter than naming it.)
         workspace = q.new_empty(max(need, 0) // 2)
@@ -258,7 +259,8 @@ class SteelCache:
             raise SteelError(status, "steel_cache_free")
 
     def compact(self):
-        """Move pages so that those in use have the lowest numbers -> their count, an int32 CUDA tensor [1]."""
+        """Move pages so that those in use have the lowest numbers -> their count, an int32 CUDA tensor [1]: ``live``, which the
+        next call writes again."""
         _check(self._lib.steel_cache_compact(self.handle, self.live.data_ptr(), self._stream(self.device_index)),
                "steel_cache_compact")
         return self.live

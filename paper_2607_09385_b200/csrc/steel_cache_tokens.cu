@@ -74,8 +74,8 @@ __device__ __forceinline__ Scale scale_from(const Scale &s, int lane) {
   return {__shfl_sync(0xffffffffu, s.pair, lane), __shfl_sync(0xffffffffu, s.inverse, lane), __shfl_sync(0xffffffffu, s.shift, lane)};
 }
 
-// f32(d / 15): multiplication by the rounded inverse and one correction give the rounded quotient for every significand
-// (tried for all 2^23 of them).
+// f32(d / 15): multiplication by the rounded inverse and one FMA correction (division by a constant after Markstein) give the rounded
+// quotient for every significand (tried for all 2^23 of them).
 __device__ __forceinline__ float fifteenth(float d) {
   constexpr float c = 1.f / 15.f;
   const float q = __fmul_rn(d, c);
