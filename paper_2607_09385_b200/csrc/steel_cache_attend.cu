@@ -14,16 +14,17 @@
 // tcgen05: the operands have to pass through registers to be unpacked, and 8 columns are all there is to multiply by.
 //
 // Work.  Segments (sequence, head, tile of 8 rows) stand one behind the other in steps of 32 tokens, each with what beginning and
-// ending it costs, and are dealt out in equal shares to all warps, whatever the lengths, which are read on the device.  A warp goes
+// ending it costs, and are dealt out in equal shares to all warps, whatever the lengths, which are read on the device.  (Tiles are counted
+// from seq_q, not from each sequence's queries: those that have no rows take shares and do nothing with them.)  A warp goes
 // through its share alone, with a ring of bulk copies of its own and no barrier, and writes the rows of segments that lie within
 // it.  Pieces of a segment in several warps of a CTA meet in shared memory, parts of one in several CTAs in global memory: the CTA
 // that ends the segment waits for the others' and puts them together in their order, so that the result does not depend on timing.
 //
-// What bounds it (B200, 296 CTAs of 8 warps): large batches the memory, at 4.5 bits a value, with about 530 instructions a warp
-// and step beside it (of which 160 unpack and 32 are products): 64 sequences of 2K to 32K tokens, 826 MB, in 141 to 145 us, 0.87
-// to 0.90 of the measured copy rate (163 us where the power limit holds).  Small ones the latency of what follows one another: slot,
+// What bounds it (B200, 296 CTAs of 8 warps): large batches the memory, at 4.5 bits a value, with about 545 instructions a warp
+// and step beside it (of which 160 unpack and 32 are products): 64 sequences of 2K to 32K tokens, 826 MB, in 143 to 156 us, 0.81
+// to 0.88 of the measured copy rate (164 us where the power limit holds).  Small ones the latency of what follows one another: slot,
 // length, page, copy (6 us until the first products), the pieces' meeting (2 to 3 us), the joining of parts (2 to 4 us): 8 x 6001
-// tokens in 22 us, of which the memory takes 8.5.
+// tokens in 22.7 us, of which the memory takes 8.5.
 //
 // Exactness.  Scores, statistics and sums are in 32 bits; Q is exact in fp16 after a power of two per row (what lies 2^-28 below a
 // row's largest entry is rounded).  P times a group's scale is rounded to fp16: 2^-11 of each product, against 2^-8 of the bf16 result.  The

@@ -4,9 +4,9 @@
 // in memory: for K the channels 32c + 8t ... + 7 of tokens g and 8 + g, for V the channels 8g ... 8g + 7 of every group of tokens
 // 8h + 2t + f.  Codes then move as 16 bytes a lane, 512 bytes a warp and group.  The lanes that share a token reduce its minimum and maximum
 // so that each ends with one token's, makes that one's scale and gives it to the others (all scales in all lanes: 28.0 us for what
-// now takes 26.5).  Memory's part is 4 head_dim bytes of bf16 and 1.125 head_dim of codes and scales a token and head;
-// quantising costs 17 instructions a value and lane (2135 a unit at head_dim 128), which is more than that leaves time for: 16K
-// tokens x 8 heads take 26.5 us against 13.1 at the measured copy rate, and reading them back 16.3.  The code is kept small, a loop over
+// then took 26.5, now 26.9).  Memory's part is 4 head_dim bytes of bf16 and 1.125 head_dim of codes and scales a token and head;
+// quantising costs 17 instructions a value and lane (2140 a unit at head_dim 128), which is more than that leaves time for: 16K
+// tokens x 8 heads take 26.9 us against 13.1 at the measured copy rate, and reading them back 16.2.  The code is kept small, a loop over
 // the groups: unrolled, most of the time went into fetching instructions (66 us).
 // Few tokens: a warp takes one token of one head, a lane four channels, 16 bits of codes.  Bound by the latency of the reads that follow
 // one another (slot, length, page) and by how much code there is to fetch: 64 sequences x 1 token written and read back in 5.0 us, with units
