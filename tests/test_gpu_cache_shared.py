@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("heads,seq", [(2, 1), (2, 5), (2, 40), (100, 40)])  # a warp a token, and a warp a unit
+@pytest.mark.parametrize("heads,seq", [(2, 1), (2, 5), (2, 40), (100, 40), (300, 40)])  # a warp a token; the last a warp a unit
 def test_append_leaves_shared_pages_alone(d, heads, seq):
     page, bad = 32, B.STEEL_ERR_INVALID_ARG
     c = make_cache(2, 40, page, heads, d, 4, 8)
